@@ -14,7 +14,8 @@
 // operand of O^T.  With V stored eight tokens of a channel together, keys,
 // probabilities and values all go from memory to the matrix cores in
 // registers, without LDS.  The softmax is the running one (maximum and sum in
-// float32, one pass); waves and parts are joined by their maxima and sums.
+// float32, one pass); waves and parts are joined by their maxima and sums,
+// which carry the factor of STEP_SHIFT with f16 elements.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(256) k_attn_part(AttnArgs p) {
     }
     float pr[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pr[e] = exp2_f(x[e] - ref);
+    for (int e = 0; e < 8; ++e) pr[e] = step_weight<F16>(x[e] - ref);
     ls += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
     const uint4 pb = make_uint4(pack2<F16>(pr[0], pr[1]), pack2<F16>(pr[2], pr[3]),
                                 pack2<F16>(pr[4], pr[5]), pack2<F16>(pr[6], pr[7]));
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(256) k_attn_part(AttnArgs p) {
       y.x = pack2<F16>(o[0] * inv, o[1] * inv);
       y.y = pack2<F16>(o[2] * inv, o[3] * inv);
       *(uint2*)((uint16_t*)p.o + ((size_t)sp.b * p.Hq + q) * D + d4) = y;
-      if (p.lse && d4 == 0) p.lse[(size_t)sp.b * p.Hq + q] = (top + log2f(l)) * LN2;
+      if (p.lse && d4 == 0) p.lse[(size_t)sp.b * p.Hq + q] = (top + (log2f(l) - STEP_SHIFT<F16>)) * LN2;
     } else {
       const size_t at = (size_t)(sp.first + sp.s) * p.Hq + q;
       *(f32x4*)&p.part_o[at * D + d4] = o;
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs p) {
     y.x = pack2<F16>(o[0] * inv, o[1] * inv);
     y.y = pack2<F16>(o[2] * inv, o[3] * inv);
     *(uint2*)((uint16_t*)p.o + ((size_t)b * p.Hq + q) * p.d + d4) = y;
-    if (p.lse && d4 == 0) p.lse[(size_t)b * p.Hq + q] = (top + log2f(l)) * LN2;
+    if (p.lse && d4 == 0) p.lse[(size_t)b * p.Hq + q] = (top + (log2f(l) - STEP_SHIFT<F16>)) * LN2;
   }
 }
 

@@ -186,6 +186,19 @@ __device__ __forceinline__ int32_t load_uniform(const int32_t* p) {
 
 __device__ __forceinline__ float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Weight of a score d octaves below its reference.  Weights that meet the
+// values in f16 are formed 2^15 too large, and with them the sums that divide
+// the result: between 2^15 and f16's smallest number lie forty octaves instead
+// of twenty-five, so that a great many small weights beside a large one keep
+// their bits (relative 2^-11 down to 2^-29 of the largest, 2^-40 of it below).
+template <int F16>
+constexpr float STEP_SHIFT = F16 ? 15.f : 0.f;
+template <int F16>
+__device__ __forceinline__ float step_weight(float d) {
+  if constexpr (F16) return exp2_f(d + STEP_SHIFT<F16>);
+  return exp2_f(d);
+}
+
 // Maximum and sum over the four lanes l % 16 + 16 i (the token groups of a
 // column of an MFMA result).
 __device__ __forceinline__ float max_groups(float v) {

@@ -465,10 +465,9 @@ size_t kda_latent_workspace_bytes(const kda_latent_config* cfg);
  * reads each cached row once for all heads:
  *   s_t = scale ((q_n W_uk) c_t + q_r r_t),  o = W_uv sum_t softmax(s)_t c_t.
  * q_n W_uk and the weighted sum of the c_t enter their products as two 16-bit
- * parts each (hi and lo), so they add no rounding of their own.  With f16
- * elements an entry of q_n W_uk past 65504 turns the head's output into NaN;
- * with bf16 elements the weighted means of a request's parts are kept in f16
- * (relative 2^-11, 2^-25 below 2^-14, saturated at 65504).
+ * parts each (hi and lo): relative 2^-16 in bf16, and in f16 2^-22 or 2^-25
+ * absolute.  With f16 elements an entry of q_n W_uk past 65504 turns the
+ * head's output into NaN.
  * In:  q_n: B rows of H vectors of d_n, q_r: B rows of H vectors of d_r, with
  *      row and head strides (in elements, multiples of 8); w_uk [H][d_n][d_c],
  *      w_uv [H][d_v][d_c]; cache, tables, lens as above.

@@ -36,24 +36,6 @@ __device__ __forceinline__ uint2 read_tr(const uint8_t* at) {
 }
 __device__ __forceinline__ uint4 join_tr(uint2 a, uint2 b) { return make_uint4(a.x, a.y, b.x, b.y); }
 
-__device__ __forceinline__ float sat16(float x) {   // NaN stays NaN
-  return x != x ? x : __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f);
-}
-
-// Four channels of a part's mean as they are kept between the launches.
-template <int F16>
-struct Mean {
-  typedef f32x4 type;
-  static __device__ __forceinline__ f32x4 value(f32x4 x) { return x; }
-};
-template <>
-struct Mean<0> {
-  typedef uint2 type;
-  static __device__ __forceinline__ f32x4 value(uint2 x) {
-    return f32x4{lo_f32<1>(x.x), hi_f32<1>(x.x), lo_f32<1>(x.y), hi_f32<1>(x.y)};
-  }
-};
-
 // A linear map of the row's four low bits that keeps banks apart both for the
 // keys (16 rows of a chunk; eight of them and the next chunk of the other eight
 // are served together) and for the transposed reads (32 bytes of rows 0 .. 3
@@ -361,8 +343,7 @@ __global__ void __launch_bounds__(256, 2) k_latent_part(LatentArgs p) {
     if (start >= end) sm[16 * ht + m] = NEG_INF;
   }
   __syncthreads();
-  // the part's means: float32 for f16 elements; for bf16 elements f16, three
-  // bits more than their type (saturated), which halves what the join reads
+  // the part's means, in float32 as every sum that is joined later
   const size_t at = (size_t)item * p.H;
 #pragma unroll
   for (int n = 0; n < NH; ++n) {
@@ -370,18 +351,8 @@ __global__ void __launch_bounds__(256, 2) k_latent_part(LatentArgs p) {
     if (h >= p.H) continue;
     const float l = sl[16 * n + m], inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int i = 0; i < DT; ++i) {
-      const f32x4 x = acc[n][i] * inv;
-      const size_t e = (at + h) * DC + 16 * (w * DT + i) + 4 * g;
-      if constexpr (F16) {
-        *(f32x4*)((float*)p.part_o + e) = x;
-      } else {
-        uint2 y;
-        y.x = pack2<1>(sat16(x[0]), sat16(x[1]));
-        y.y = pack2<1>(sat16(x[2]), sat16(x[3]));
-        *(uint2*)((uint16_t*)p.part_o + e) = y;
-      }
-    }
+    for (int i = 0; i < DT; ++i)
+      *(f32x4*)&p.part_o[(at + h) * DC + 16 * (w * DT + i) + 4 * g] = acc[n][i] * inv;
   }
   for (int e = t; e < NH * 16; e += NW * WAVE)
     if (h0 + e < p.H) *(float2*)&p.part_ml[(at + h0 + e) * 2] = make_float2(sm[e], sl[e]);
@@ -419,14 +390,12 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
     const size_t at = (size_t)sp.first * p.H + h;
     const float2* ml = (const float2*)p.part_ml + at;
     const int s0 = w & ((1 << wl) - 1), ds = 1 << wl;
-    // four channels of a part's mean
-    typedef typename Mean<F16>::type Part;
-    const Part* from = (const Part*)p.part_o + (at * DC + 4 * lane) / 4;
+    const f32x4* from = (const f32x4*)p.part_o + at * (DC / 4) + lane;
     const auto part = [&](int s, int u) { return from[(size_t)s * p.H * (DC / 4) + 64 * u]; };
     // of part `lane`; the first parts are on their way while their weights are formed
     float2 mine = make_float2(NEG_INF, 0.f);
     if (lane < sp.ns) mine = ml[(size_t)lane * p.H];
-    Part ahead[4][PER];
+    f32x4 ahead[4][PER];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -459,14 +428,14 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
       if (s < sp.ns) {
         const float f = weight(s);
 #pragma unroll
-        for (int u = 0; u < PER; ++u) o[u] += Mean<F16>::value(ahead[i][u]) * f;
+        for (int u = 0; u < PER; ++u) o[u] += ahead[i][u] * f;
       }
     }
 #pragma unroll 2
     for (int s = s0 + 4 * ds; s < sp.ns; s += ds) {
       const float f = weight(s);
 #pragma unroll
-      for (int u = 0; u < PER; ++u) o[u] += Mean<F16>::value(part(s, u)) * f;
+      for (int u = 0; u < PER; ++u) o[u] += part(s, u) * f;
     }
   }
 #pragma unroll

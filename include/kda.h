@@ -465,8 +465,8 @@ size_t kda_latent_workspace_bytes(const kda_latent_config* cfg);
  * reads each cached row once for all heads:
  *   s_t = scale ((q_n W_uk) c_t + q_r r_t),  o = W_uv sum_t softmax(s)_t c_t.
  * q_n W_uk and the weighted sum of the c_t enter their products as two 16-bit
- * parts each (hi and lo): relative 2^-16 in bf16, and in f16 2^-22 or 2^-25
- * absolute.  With f16 elements an entry of q_n W_uk past 65504 turns the
+ * parts each (hi and lo): relative 2^-16 in bf16, and in f16 2^-22 or
+ * absolute 2^-25 (the queries) and 2^-36 (the sum).  With f16 elements an entry of q_n W_uk past 65504 turns the
  * head's output into NaN.
  * In:  q_n: B rows of H vectors of d_n, q_r: B rows of H vectors of d_r, with
  *      row and head strides (in elements, multiples of 8); w_uk [H][d_n][d_c],

@@ -45,14 +45,21 @@ __device__ __forceinline__ int row_swizzle(int i) {
   return (i & 3) << 1 | (((i >> 2) ^ (i >> 3)) & 1) << 3 | ((i >> 3) & 1);
 }
 
-// Four floats as hi and lo 16-bit parts.
+// Four floats as hi and lo 16-bit parts, the lo part times `up`.
 template <int F16>
-__device__ __forceinline__ void split4(const f32x4& x, uint2& hi, uint2& lo) {
+__device__ __forceinline__ void split4(const f32x4& x, uint2& hi, uint2& lo, float up = 1.f) {
   hi.x = pack2<F16>(x[0], x[1]);
   hi.y = pack2<F16>(x[2], x[3]);
-  lo.x = pack2<F16>(x[0] - lo_f32<F16>(hi.x), x[1] - hi_f32<F16>(hi.x));
-  lo.y = pack2<F16>(x[2] - lo_f32<F16>(hi.y), x[3] - hi_f32<F16>(hi.y));
+  lo.x = pack2<F16>((x[0] - lo_f32<F16>(hi.x)) * up, (x[1] - hi_f32<F16>(hi.x)) * up);
+  lo.y = pack2<F16>((x[2] - lo_f32<F16>(hi.y)) * up, (x[3] - hi_f32<F16>(hi.y)) * up);
 }
+
+// The joined sums are small where a token of large weight has a small latent
+// vector.  Their lo part in f16 is formed 2^11 too large (the half step of
+// 65504 still fits) and its product scaled down again: the pair then ends at
+// 2^-36 instead of 2^-25.
+template <int F16>
+constexpr float LO_UP = F16 ? 2048.f : 1.f;
 
 }  // namespace
 
@@ -446,18 +453,18 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
     f32x4 x = *(const f32x4*)&sums[r << wl][c4];
     for (int i = 1; i < 1 << wl; ++i) x += *(const f32x4*)&sums[(r << wl) + i][c4];
     uint2 hi, lo;
-    split4<F16>(x, hi, lo);
+    split4<F16>(x, hi, lo, LO_UP<F16>);
     *(uint2*)&mid[0][r * OS + c4] = hi;
     *(uint2*)&mid[1][r * OS + c4] = lo;
   }
   __syncthreads();
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int x0 = m * OS + 32 * KS * kp + 8 * g;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    const int x = m * OS + 32 * (KS * kp + ks) + 8 * g;
-    acc = mma16<F16>(a[ks], *(const uint4*)&mid[1][x], acc);
-    acc = mma16<F16>(a[ks], *(const uint4*)&mid[0][x], acc);
-  }
+  for (int ks = 0; ks < KS; ++ks) acc = mma16<F16>(a[ks], *(const uint4*)&mid[1][x0 + 32 * ks], acc);
+  if constexpr (F16) acc *= 1.f / LO_UP<F16>;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) acc = mma16<F16>(a[ks], *(const uint4*)&mid[0][x0 + 32 * ks], acc);
   *(f32x4*)&sums[w][4 * lane] = acc;   // the joined sums have been read
   __syncthreads();
   if (kp == 0 && m < nb) {

@@ -14,7 +14,8 @@ I32 = dict(dtype=torch.int32, device="cuda")
 
 
 @pytest.mark.parametrize("dtype,size,weight", [("bf16", 2.0 ** -30, 2.0 ** 20), ("bf16", 2.0 ** -12, 2.0 ** 10),
-                                               ("bf16", 2.0 ** 40, 2.0 ** -40)])
+                                               ("bf16", 2.0 ** 40, 2.0 ** -40), ("f16", 2.0 ** -22, 2.0 ** 14),
+                                               ("f16", 2.0 ** -14, 2.0 ** 12), ("f16", 2.0 ** 14, 2.0 ** -8)])
 @pytest.mark.parametrize("lens", [[40, 1], [3000, 130, 0, 900]], ids=str)
 def test_step_means_of_any_size(dtype, size, weight, lens):
     H, dn, dr, dc, page = 17, 64, 32, 256, 64

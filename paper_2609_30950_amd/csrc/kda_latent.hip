@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256, 2) k_latent_part(LatentArgs p) {
     for (int ti = 0; ti < 2; ++ti) {
       float pr[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) pr[r] = exp2_f(x[4 * ti + r] - ref);
+      for (int r = 0; r < 4; ++r) pr[r] = step_weight<F16>(x[4 * ti + r] - ref);
       own_l += (pr[0] + pr[1]) + (pr[2] + pr[3]);
       if (ti % KW == kw) {
         uint2 y;

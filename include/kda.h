@@ -347,8 +347,8 @@ int kda_prefill_aux(const kda_config* cfg, int32_t T, int32_t C, void* records,
  *   otherwise).
  * - Scores, softmax sums and accumulators are float32.  The probabilities meet
  *   the values in a 16-bit type: relative rounding 2^-8 in bf16, and in f16
- *   2^-11 down to 2^-29 of the largest one, below that 2^-40 of the largest;
- *   the sums they are divided by are not rounded.
+ *   2^-11 down to 2^-29 of the largest one, below that 2^-40 of the largest
+ *   (prompts: see there); the sums they are divided by are not rounded.
  * - Outputs and workspaces overlap no input.  A call reads nothing that an
  *   earlier call left in a workspace.
  * ------------------------------------------------------------------------ */
@@ -486,8 +486,9 @@ size_t kda_latent_prefill_workspace_bytes(const kda_latent_config* cfg, int32_t 
  * .. cu[b+1] - 1, which are its last tokens (append first), attend to its
  * cached tokens up to themselves.  Keys, values, queries and the shared parts
  * are rounded to f16 (relative 2^-11, 2^-25 below 2^-14, saturated at 65504;
- * with f16 elements keys to hi + lo).  Rows from
- * min(cu[B], n) on are left as they were.
+ * with f16 elements keys to hi + lo), and so are the probabilities (relative
+ * 2^-11 down to 2^-25 of the largest one, below that 2^-36 of the largest).
+ * Rows from min(cu[B], n) on are left as they were.
  * n, max_kv: at most 2^22.  max_kv is an upper bound of the tokens (lens) of
  *      the requests that have rows, summed; the rows of requests past it are
  *      filled with NaN.  A request

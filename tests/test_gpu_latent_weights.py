@@ -72,3 +72,26 @@ def test_step_one_large_score(dtype, drop):
     worst = max(_share(s["o"][b], s["vals"][b], at[b], n, drop, dtype, floor, u + u * u) for b, n in enumerate(lens))
     say(f"small weights 2^-{drop} latent step {dtype}: {worst:.3f} of the bound")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dn", [64, 128])
+@pytest.mark.parametrize("drop", [3.75, 7.5, 15.5, 20.5, 25.25, 30.0])
+def test_prompts_one_large_score(dtype, dn, drop):
+    """Chains in one block, in parts, and the large score first, amid and last."""
+    for lens, at, rows in (([700, 90, 33], [0, 60, 32], [130, 90, 33]), ([5000], [0], [3]), ([5000], [2222], [3]),
+                           ([1500], [1499], [2])):
+        s = _world(lens, at, drop, dtype, rows, dn)
+        cu = [sum(rows[:b]) for b in range(len(rows) + 1)]
+        K.kda_latent_prefill(s["cfg"], sum(lens), s["q_n"], s["q_r"], torch.tensor(cu, **I32), s["w_uk"], s["w_uv"],
+                             s["cache"], s["tables"], s["lens"], s["o"],
+                             K.new_latent_prefill_workspace(s["cfg"], sum(lens)))
+        torch.cuda.synchronize()
+        worst = 0.0
+        for b, n in enumerate(lens):
+            for i in range(rows[b]):
+                seen = n - rows[b] + i + 1
+                worst = max(worst, _share(s["o"][cu[b] + i], s["vals"][b], at[b], seen, drop, dtype, 2.0 ** -36,
+                                          2 * 2.0 ** -11 * (1 + 2.0 ** -11)))
+        say(f"small weights 2^-{drop} prompts {dtype} d={dn} {lens}: {worst:.3f} of the bound")
+        assert worst <= 1.0

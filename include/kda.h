@@ -485,9 +485,11 @@ size_t kda_latent_prefill_workspace_bytes(const kda_latent_config* cfg, int32_t 
  * head are formed once from the cached rows, and the rows of request b, cu[b]
  * .. cu[b+1] - 1, which are its last tokens (append first), attend to its
  * cached tokens up to themselves.  Keys, values, queries and the shared parts
- * are rounded to f16 (relative 2^-11, 2^-25 below 2^-14, saturated at 65504;
- * with f16 elements keys to hi + lo), and so are the probabilities (relative
+ * are rounded to f16 (relative 2^-11, 2^-25 below 2^-14, finite numbers cut
+ * to 65504; with f16 elements keys to hi + lo), and so are the probabilities (relative
  * 2^-11 down to 2^-25 of the largest one, below that 2^-36 of the largest).
+ * A token whose c is not finite makes the rows that see it NaN, a row of w_uv
+ * that is not finite its channel of all rows that have tokens.
  * Rows from min(cu[B], n) on are left as they were.
  * n, max_kv: at most 2^22.  max_kv is an upper bound of the tokens (lens) of
  *      the requests that have rows, summed; the rows of requests past it are

@@ -76,6 +76,7 @@ struct LatentPrefillArgs {
   int kv_rows;                  // rows of the expanded arrays, a multiple of 256
   int32_t* src;                 // [kv_rows] cached row of each packed token, -1: no such page
   int32_t* lay;                 // off [B + 1], kvn [B], qoff [B + 1]
+  int32_t* gone;                // [H][d_v / 32] bits of the value channels whose weights are not finite
   // f16: keys [H][kv_rows][d_n] (f16 elements: [2][H]..., hi and lo), shared parts [kv_rows][d_r], values [H][kv_rows / 8][d_v][8]
   void *ke, *re, *ve;
   int parts;                    // parts that a query tile's tokens are cut into

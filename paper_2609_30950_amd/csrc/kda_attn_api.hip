@@ -151,7 +151,7 @@ int prefill_parts(const kda_latent_config* cfg, int n, int max_kv) {
 
 struct PrefillWs {
   int kv_rows;
-  size_t lay_off, src_off, k_off, r_off, v_off, o_off, ml_off, rows_off, total;
+  size_t lay_off, gone_off, src_off, k_off, r_off, v_off, o_off, ml_off, rows_off, total;
 };
 
 // Requests start at multiples of 8 tokens, tiles of 64 tokens may read past
@@ -162,7 +162,8 @@ PrefillWs prefill_ws(const kda_latent_config* cfg, int max_kv) {
   w.kv_rows = (max_kv + 7 * parts + 64 + 255) / 256 * 256;
   const size_t rows = (size_t)w.kv_rows;
   w.lay_off = 0;
-  w.src_off = up256((size_t)(3 * cfg->pg.B + 2) * sizeof(int32_t));
+  w.gone_off = up256((size_t)(3 * cfg->pg.B + 2) * sizeof(int32_t));
+  w.src_off = up256(w.gone_off + (size_t)cfg->H * cfg->d_v / 32 * sizeof(int32_t));
   w.k_off = up256(w.src_off + rows * sizeof(int32_t));
   w.r_off = up256(w.k_off + rows * cfg->H * cfg->d_n * 2 * (cfg->dtype == KDA_F16 ? 2 : 1));   // hi (and lo) keys
   w.v_off = up256(w.r_off + rows * cfg->d_r * 2);
@@ -433,6 +434,7 @@ int kda_latent_prefill(const kda_latent_config* cfg, int32_t n, int32_t max_kv, 
   const PrefillWs w = prefill_ws(cfg, max_kv);
   a.kv_rows = w.kv_rows;
   a.lay = (int32_t*)((uint8_t*)ws + w.lay_off);
+  a.gone = (int32_t*)((uint8_t*)ws + w.gone_off);
   a.src = (int32_t*)((uint8_t*)ws + w.src_off);
   a.ke = (uint8_t*)ws + w.k_off;
   a.re = (uint8_t*)ws + w.r_off;

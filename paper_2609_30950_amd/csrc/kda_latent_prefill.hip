@@ -14,7 +14,15 @@
 // rounding of the output.  For f16 elements keys and probabilities are pairs
 // hi + lo instead, and the values' rounding is the only one beside the
 // output's (single keys and probabilities gave twice the output's rounding;
-// the pairs take twice the products).  Everything is saturated at 65504.
+// the pairs take twice the products).  Finite numbers are saturated at 65504.
+//
+// A product with the values meets all tokens of a tile, those that a row does
+// not see with weight zero, which must not become NaN: the expanded values are
+// finite whatever they are formed from.  A latent vector that is not has keys
+// that are not either, in every head and channel; they are stored as NaN and
+// reach the rows that see the token through its scores.  Weights W_uv that are
+// not finite belong to a channel and not to a token: k_latent_rows notes those
+// channels, which become NaN at the end.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -37,8 +45,11 @@ constexpr int KT = 64;    // tokens of a tile
 // longer lag rescales less often: long prompts 868 us with 4, 864 with 8.
 constexpr float SHIFT = 11.f, LAG = 4.f;
 
-__device__ __forceinline__ float sat16(float x) {   // NaN stays NaN
-  return x != x ? x : __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f);
+__device__ __forceinline__ float sat16(float x) {   // infinities and NaN stay
+  return __builtin_isfinite(x) ? __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f) : x;
+}
+__device__ __forceinline__ float sat16_or_nan(float x) {
+  return __builtin_isfinite(x) ? __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f) : __builtin_nanf("");
 }
 __device__ __forceinline__ float sat16_or_0(float x) {
   return x != x ? 0.f : __builtin_amdgcn_fmed3f(x, -65504.f, 65504.f);
@@ -92,14 +103,43 @@ __device__ __forceinline__ int block_before(int v, int most, int* part) {
   return before;
 }
 
+// Bit i: row i of 32 rows of dc (256 or 512) elements holds one that is not
+// finite, the exponent's bits all set.  A load covers 512 elements.
+template <int F16>
+__device__ __forceinline__ uint32_t not_finite_rows(const uint16_t* from, int dc) {
+  constexpr uint32_t EXP = F16 ? 0x7C007C00u : 0x7F807F80u, ONE = F16 ? 0x04000400u : 0x00800080u;
+  const uint4* at = (const uint4*)from + lane_id();
+  uint32_t bits = 0u;
+  for (int i0 = 0; i0 < dc / 16; i0 += 16) {   // of the loads that the rows take, 16 or 32
+    uint4 v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = at[WAVE * (i0 + i)];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t all = ((v[i].x & EXP) + ONE) | ((v[i].y & EXP) + ONE) | ((v[i].z & EXP) + ONE) | ((v[i].w & EXP) + ONE);
+      const unsigned long long who = __ballot((all & 0x80008000u) != 0u);
+      if (dc == 512) bits |= (uint32_t)(who != 0) << (i0 + i);
+      else bits |= (uint32_t)((uint32_t)who != 0u) << (2 * i) | (uint32_t)((who >> 32) != 0) << (2 * i + 1);
+    }
+  }
+  return bits;
+}
+
 // Packs the requests that have rows: their tokens from multiples of 8 on
 // (off), the tokens held (kvn; -1 where the sum of the lengths has passed
 // max_kv) and their query tiles (qoff); and for every packed token its cached
 // row (src; -1 on a page that does not exist) and its shared key part as f16.
 // Each block forms the sums over the requests by itself (thread t holds the
 // consecutive requests t R ..), which costs less than a launch before this one.
+// The blocks from `row_blocks` on look for weights of the values that are not
+// finite, a wave at 32 rows of W_uv (32 value channels of a head).
 template <int F16, int R>
-__global__ void __launch_bounds__(256) k_latent_rows(LatentPrefillArgs p) {
+__global__ void __launch_bounds__(256) k_latent_rows(LatentPrefillArgs p, int row_blocks) {
+  if ((int)blockIdx.x >= row_blocks) {
+    const int word = __builtin_amdgcn_readfirstlane(4 * ((int)blockIdx.x - row_blocks) + (int)threadIdx.x / WAVE);
+    if (word < p.H * p.dn / 32) p.gone[word] = not_finite_rows<F16>((const uint16_t*)p.w_uv + (size_t)word * 32 * p.dc, p.dc);
+    return;
+  }
   __shared__ int part[3][4], s_off[256 * R], s_kvn[256 * R];
   const int t = threadIdx.x, B = p.pg.B, cap = p.pg.max_pages << p.sh, most = p.max_kv + 1;
   int len[R], tiles[R], sum = 0;
@@ -266,8 +306,7 @@ __global__ void __launch_bounds__(256, TX == 128 ? 3 : 2) k_latent_expand(Latent
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const float a = acc[k][i][j][2 * u], b = acc[k][i][j][2 * u + 1];
-          // a token's NaN comes back through the scores
-          y[2 * i + u] = values ? pack2<1>(sat16_or_0(a), sat16_or_0(b)) : pack2<1>(sat16(a), sat16(b));
+          y[2 * i + u] = values ? pack2<1>(sat16_or_0(a), sat16_or_0(b)) : pack2<1>(sat16_or_nan(a), sat16_or_nan(b));
         }
       if (col >= cols) continue;
       const size_t h = col / DN, d = col % DN;
@@ -601,7 +640,13 @@ __global__ void __launch_bounds__(256 * TS, F16 || TS == 2 ? 1 : 2) k_latent_att
   }
   if (r < last) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < NT; ++i) {
+      const uint32_t gone = load_uniform(p.gone + h * NT + i);
+      if (gone != 0 && l != 0.f) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (gone >> (8 * (e >> 2) + 4 * hh + (e & 3)) & 1) acc[i][e] = __builtin_nanf("");
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint2 y;
@@ -609,6 +654,7 @@ __global__ void __launch_bounds__(256 * TS, F16 || TS == 2 ? 1 : 2) k_latent_att
         y.y = pack2<F16>(acc[i][4 * k + 2] * inv, acc[i][4 * k + 3] * inv);
         *(uint2*)&o[((size_t)r * p.H + h) * DN + 32 * i + 8 * k + 4 * hh] = y;
       }
+    }
   }
 }
 
@@ -649,7 +695,13 @@ __global__ void __launch_bounds__(256) k_latent_attend_join(LatentPrefillArgs p)
   rl[v][lane] = l;
   __syncthreads();
   l = (rl[0][lane] + rl[1][lane]) + (rl[2][lane] + rl[3][lane]);
-  const f32x4 x = (red[0][v][lane] + red[1][v][lane]) + (red[2][v][lane] + red[3][v][lane]);
+  f32x4 x = (red[0][v][lane] + red[1][v][lane]) + (red[2][v][lane] + red[3][v][lane]);
+  const uint32_t gone = load_uniform(p.gone + h * NT + i);
+  if (gone != 0 && l != 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (gone >> (8 * v + 4 * hh + e) & 1) x[e] = __builtin_nanf("");
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int r = q0 + 32 * w + c;
   if (r >= last) return;
@@ -689,8 +741,9 @@ hipError_t launch_attend(const LatentPrefillArgs& a, hipStream_t st) {
 template <int F16>
 hipError_t launch_prefill_t(const LatentPrefillArgs& a, hipStream_t st) {
   const unsigned row_blocks = ((unsigned)a.kv_rows * (a.dr / 8) + 255) / 256;
-  hipError_t e = a.pg.B <= 256 ? launch("latent_rows", k_latent_rows<F16, 1>, row_blocks, 256, 0, st, a)
-                               : launch("latent_rows", k_latent_rows<F16, 16>, row_blocks, 256, 0, st, a);
+  const unsigned grid = row_blocks + ((unsigned)a.H * a.dn / 32 + 3) / 4;
+  hipError_t e = a.pg.B <= 256 ? launch("latent_rows", k_latent_rows<F16, 1>, grid, 256, 0, st, a, (int)row_blocks)
+                               : launch("latent_rows", k_latent_rows<F16, 16>, grid, 256, 0, st, a, (int)row_blocks);
   if (e != hipSuccess) return e;
   if (a.dn == 64)
     e = a.dc == 256 ? launch_expand<F16, 256, 64>(a, st) : launch_expand<F16, 512, 64>(a, st);

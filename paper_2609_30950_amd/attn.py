@@ -6,7 +6,7 @@ torch's current stream.  Row-strided inputs (slices of a fused projection)
 are taken as they are; everything else is contiguous.
 """
 import ctypes
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 from math import sqrt
 from typing import Optional
 
@@ -20,8 +20,16 @@ _E4M3 = (2, torch.float8_e4m3fn)
 _I32 = torch.int32
 
 
+class _Value:
+    """Copies and pickles are made from the fields alone (the C structure and
+    its reference are formed anew)."""
+
+    def __reduce__(self):
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
+
 @dataclass(frozen=True)
-class Pages:
+class Pages(_Value):
     """Requests and the page pool they share."""
     B: int
     page: int
@@ -40,7 +48,7 @@ def _element(cfg):
 
 
 @dataclass(frozen=True)
-class AttnConfig:
+class AttnConfig(_Value):
     """Grouped-query attention; cache "same" (as dtype) or "e4m3"."""
     pages: Pages
     H_q: int
@@ -72,7 +80,7 @@ class AttnConfig:
 
 
 @dataclass(frozen=True)
-class LatentConfig:
+class LatentConfig(_Value):
     """Latent attention: H heads over cached rows [c (d_c), r (d_r)]."""
     pages: Pages
     H: int

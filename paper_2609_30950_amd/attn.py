@@ -20,6 +20,13 @@ _E4M3 = (2, torch.float8_e4m3fn)
 _I32 = torch.int32
 
 
+def _int32(**numbers):
+    """ctypes would cut a wider number to its low 32 bits."""
+    for name, x in numbers.items():
+        if not -2**31 <= x < 2**31:
+            raise KdaError(f"{name}: {x} does not fit 32 bits")
+
+
 class _Value:
     """Copies and pickles are made from the fields alone (the C structure and
     its reference are formed anew)."""
@@ -37,6 +44,7 @@ class Pages(_Value):
     max_pages: int
 
     def __post_init__(self):
+        _int32(B=self.B, page=self.page, n_pages=self.n_pages, max_pages=self.max_pages)
         object.__setattr__(self, "_c", kda_pages(self.B, self.page, self.n_pages, self.max_pages))
         object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
@@ -63,6 +71,7 @@ class AttnConfig(_Value):
         if self.cache not in ("same", "e4m3"):
             raise KdaError(f"cache: expected 'same' or 'e4m3', got {self.cache!r}")
         held = _E4M3 if self.cache == "e4m3" else (code, t)
+        _int32(H_q=self.H_q, H_kv=self.H_kv, d=self.d)
         if self.d < 1:
             raise KdaError("invalid config")
         scale = 1.0 / sqrt(self.d) if self.scale is None else float(self.scale)
@@ -93,6 +102,7 @@ class LatentConfig(_Value):
 
     def __post_init__(self):
         code, t = _element(self)
+        _int32(H=self.H, d_n=self.d_n, d_r=self.d_r, d_c=self.d_c, d_v=self.d_v)
         if self.d_n < 1 or self.d_r < 1:
             raise KdaError("invalid config")
         scale = 1.0 / sqrt(self.d_n + self.d_r) if self.scale is None else float(self.scale)
@@ -202,6 +212,8 @@ def kda_pages_plan(pages, lens, new_tokens, n_free, free_pages, tables, lens_out
     B = pages.B
     per = (B,)
     n = slots.numel()
+    if n >= 2**31:
+        _int32(slots=n)
     _check(load().kda_pages_plan(
         pages._ref, n, _dense(lens, _I32, per, dev, "lens"), _dense(new_tokens, _I32, per, dev, "new_tokens"),
         _dense(n_free, _I32, (1,), dev, "n_free"), _dense(free_pages, _I32, (pages.n_pages,), dev, "free_pages"),
@@ -267,8 +279,13 @@ def new_latent_workspace(cfg, device="cuda"):
     return _new_workspace(cfg._need, device)
 
 
+def _prefill_bytes(cfg, max_kv):
+    _int32(max_kv=max_kv)
+    return int(load().kda_latent_prefill_workspace_bytes(cfg._ref, max_kv))
+
+
 def new_latent_prefill_workspace(cfg, max_kv, device="cuda"):
-    return _new_workspace(int(load().kda_latent_prefill_workspace_bytes(cfg._ref, max_kv)), device)
+    return _new_workspace(_prefill_bytes(cfg, max_kv), device)
 
 
 def kda_latent_append(cfg, c, r, slots, cache):
@@ -298,11 +315,11 @@ def kda_latent_prefill(cfg, max_kv, q_n, q_r, cu, w_uk, w_uv, cache, tables, len
     head-strided), request b's in cu[b] .. cu[b + 1] - 1; o [n, H, d_v]."""
     dev, stream = _here()
     t, B, H, n = cfg._t, cfg.pages.B, cfg.H, q_n.shape[0]
-    lib = load()
-    _check(lib.kda_latent_prefill(
+    need = _prefill_bytes(cfg, max_kv)
+    _check(load().kda_latent_prefill(
         cfg._ref, n, max_kv, *_heads(q_n, t, (n, H, cfg.d_n), dev, "q_n"),
         *_heads(q_r, t, (n, H, cfg.d_r), dev, "q_r"), _dense(cu, _I32, (B + 1,), dev, "cu"),
         _dense(w_uk, t, cfg._uk, dev, "w_uk"), _dense(w_uv, t, cfg._uv, dev, "w_uv"),
         _dense(cache, t, cfg.cache_shape, dev, "cache"), _dense(tables, _I32, cfg._table, dev, "tables"),
         _dense(lens, _I32, (B,), dev, "lens"), _dense(o, t, (n, H, cfg.d_v), dev, "o"),
-        _scratch(ws, int(lib.kda_latent_prefill_workspace_bytes(cfg._ref, max_kv)), dev), stream))
+        _scratch(ws, need, dev), stream))

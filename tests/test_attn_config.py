@@ -26,3 +26,19 @@ def test_configs_are_copied_and_sent(cfg):
             assert getattr(other, name, None) == getattr(cfg, name, None)
         if hasattr(other, "pages"):
             assert other.pages == PAGES
+
+
+W = 2**32
+
+
+@pytest.mark.parametrize("make", [
+    lambda: K.Pages(W + 2, 64, 8, 4), lambda: K.Pages(2, W + 64, 8, 4), lambda: K.Pages(2, 64, W + 8, 4),
+    lambda: K.Pages(2, 64, 8, W + 4), lambda: K.AttnConfig(PAGES, W + 4, 2, 64),
+    lambda: K.AttnConfig(PAGES, 4, W + 2, 64), lambda: K.AttnConfig(PAGES, 4, 2, W + 64),
+    lambda: K.LatentConfig(PAGES, W + 4, 128, 64, 512, 128), lambda: K.LatentConfig(PAGES, 4, 128, W + 64, 512, 128),
+    lambda: K.LatentConfig(PAGES, 4, 128, 64, W + 512, 128), lambda: K.LatentConfig(PAGES, 4, 128, 64, 512, 128 - W),
+    lambda: K.new_latent_prefill_workspace(K.LatentConfig(PAGES, 4, 128, 64, 512, 128), W + 100, device="cpu"),
+    lambda: K.new_latent_prefill_workspace(K.LatentConfig(PAGES, 4, 128, 64, 512, 128), 2**31, device="cpu")])
+def test_numbers_past_32_bits_are_refused(make):
+    with pytest.raises(K.KdaError):
+        make()

@@ -176,6 +176,13 @@ def _heads(t, dtype, shape, dev, name):
     _refuse(t, dtype, shape, dev, name)
 
 
+def _count(t, dim=None):
+    """Elements, or the size of a dimension; 0 for what the checks refuse."""
+    if not isinstance(t, torch.Tensor):
+        return 0
+    return t.numel() if dim is None else t.shape[dim] if t.dim() > dim else 0
+
+
 def _scratch(ws, need, dev, name="ws"):
     if need == 0:
         raise KdaError("invalid config")
@@ -211,7 +218,7 @@ def kda_pages_plan(pages, lens, new_tokens, n_free, free_pages, tables, lens_out
     dev, stream = _here()
     B = pages.B
     per = (B,)
-    n = slots.numel()
+    n = _count(slots)
     if n >= 2**31:
         _int32(slots=n)
     _check(load().kda_pages_plan(
@@ -247,7 +254,7 @@ def kda_attn_append(cfg, k, v, slots, k_cache, v_cache, k_scale=None, v_scale=No
     """Rows k, v [n, H_kv, d] (row-strided) into the pages of slots [n]."""
     _only_e4m3(cfg, k_scale, v_scale)
     dev, stream = _here()
-    n = slots.numel()
+    n = _count(slots)
     shape = (n, cfg.H_kv, cfg.d)
     ks, vs = _scales(cfg, k_scale, v_scale, dev)
     _check(load().kda_attn_append(
@@ -291,7 +298,7 @@ def new_latent_prefill_workspace(cfg, max_kv, device="cuda"):
 def kda_latent_append(cfg, c, r, slots, cache):
     """Rows c [n, d_c] and r [n, d_r] (row-strided) into the pages of slots [n]."""
     dev, stream = _here()
-    n = slots.numel()
+    n = _count(slots)
     _check(load().kda_latent_append(
         cfg._ref, n, *_rows(c, cfg._t, (n, cfg.d_c), dev, "c"), *_rows(r, cfg._t, (n, cfg.d_r), dev, "r"),
         _dense(slots, _I32, (n,), dev, "slots"), _dense(cache, cfg._t, cfg.cache_shape, dev, "cache"), stream))
@@ -314,7 +321,7 @@ def kda_latent_prefill(cfg, max_kv, q_n, q_r, cu, w_uk, w_uv, cache, tables, len
     """Packed prompt rows q_n [n, H, d_n], q_r [n, H, d_r] (row- and
     head-strided), request b's in cu[b] .. cu[b + 1] - 1; o [n, H, d_v]."""
     dev, stream = _here()
-    t, B, H, n = cfg._t, cfg.pages.B, cfg.H, q_n.shape[0]
+    t, B, H, n = cfg._t, cfg.pages.B, cfg.H, _count(q_n, 0)
     need = _prefill_bytes(cfg, max_kv)
     _check(load().kda_latent_prefill(
         cfg._ref, n, max_kv, *_heads(q_n, t, (n, H, cfg.d_n), dev, "q_n"),

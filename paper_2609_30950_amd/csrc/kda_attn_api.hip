@@ -97,14 +97,19 @@ int check_latent(const kda_latent_config* cfg) {
   return KDA_OK;
 }
 
-// The chip holds 512 blocks at once, two a compute unit.  The parts are cut so
-// that those of a large batch fit that (128 requests up to 4000 tokens, 32
-// heads, a whole step: 77 us, 88 where they do not; 64 requests up to 8192: 71
-// us, with 256 blocks 84), and a block a compute unit does for few requests,
-// which are not ragged and whose join grows with the parts (8 requests up to
-// 16000 tokens, 32 heads: 43 us, with 512 blocks 60; 1 of 60000: 50 and 69).
-// No part below 64 tokens: with 32 the join pays what the parts gain (one
-// request of 2001 tokens: 19.4 and 19.6 us).
+// The chip holds 512 blocks at once, two a compute unit.  With up to 32 heads a
+// part is a block, and the parts of a large batch are cut so that they fit that
+// (whole steps, 32 heads, bf16: 128 requests up to 4000 tokens 80 us, 93 with
+// 512 parts besides one a request and 86 with 256; 64 requests up to 8192: 74,
+// 75 and 86).  With more heads a part has a block per 32 of them, which read
+// the same rows; as many blocks are then past the 512, and still this is the
+// faster cut: 512 less a batch's B ceil(H / 32) blocks takes 135 us against 109
+// (128 requests up to 4000, 64 heads), 223 against 187 (64 up to 8000, 128
+// heads).  A block a compute unit does for few requests, which are not ragged
+// and whose join grows with the parts (32 heads, 8 requests up to 16000 tokens:
+// 43 us, with 512 blocks 64; 1 of 60000: 51 and 73).  No part below 64 tokens:
+// with 32 the join pays what the parts gain (one request of 2001 tokens: 19.4
+// and 19.6 us), with 128 there are too few (23.1 against 19.8 us).
 int latent_blocks(int B) {
   const int few = 16 * B > 256 ? 16 * B : 256, many = B < 256 ? 512 - B : 256;
   return few < many ? few : many;

@@ -349,7 +349,8 @@ int kda_prefill_aux(const kda_config* cfg, int32_t T, int32_t C, void* records,
  *   the values in a 16-bit type: relative rounding 2^-8 in bf16, and in f16
  *   2^-11 down to 2^-29 of the largest one, below that 2^-40 of the largest
  *   (prompts: see there); the sums they are divided by are not rounded.
- * - Outputs and workspaces overlap no input.  A call reads nothing that an
+ * - Counts are at least 1: a step without rows makes no call (KDA_ERR_ARG).
+ * - Outputs and workspaces overlap no input but where it is said.  A call reads nothing that an
  *   earlier call left in a workspace.
  * ------------------------------------------------------------------------ */
 
@@ -391,9 +392,9 @@ typedef struct {
   double scale;   /* factor of the scores, below 2^127 in magnitude           */
 } kda_latent_config;
 
-/* Block tables and slot maps of one serving step (n_slots at most 2^24, the
- * rows an append may have).  new_tokens[b] says what
- * request b does: n > 0 appends n tokens, 0 waits, below 0 ends.
+/* Block tables and slot maps of one serving step (n_slots from 1 to 2^24, the
+ * rows an append may have).  new_tokens[b] says what request b does: n > 0
+ * appends n tokens, 0 waits, below 0 ends.
  *   1. Ended requests return their ceil(lens / page) pages: pushed onto the
  *      free stack in request order, each request's pages in table order.
  *   2. Requests with new tokens are admitted in request order as long as the
@@ -403,7 +404,7 @@ typedef struct {
  *      (and takes nothing) if it would exceed max_pages, if its rows lie past
  *      n_slots, or if its length is out of range.  The i-th page taken is the
  *      i-th from the top of the stack, appended to its request's table row.
- *   3. cu[b] = sum of max(new, 0) of the requests before b (the rows of
+ *   3. cu[b] = sum of max(new, 0) of the requests before b (2^31 - 1 at most; the rows of
  *      request b are cu[b] .. cu[b+1] - 1 whether admitted or not), and
  *      slots[row] = page id * page + offset of the row's token, or -1 for
  *      rows of refused requests and rows from cu[B] on.
@@ -413,8 +414,10 @@ typedef struct {
  *      pages are not read and not written.
  * Out: lens_out [B] (0 after the end; may be lens), n_free_out [1] (may be
  *      n_free), cu [B + 1], slots [n_slots], ok [B] (1: admitted, waiting or
- *      ended; 0: refused).  The same inputs give the same outputs and leave
- *      tables and free_pages the same, so a repeated call repeats the step.
+ *      ended; 0: refused, or waiting with a length out of range or a cu[b]
+ *      past n_slots, where there is nothing to repeat).  The same inputs give
+ *      the same outputs and leave tables and free_pages the same, so a
+ *      repeated call repeats the step.
  * A refused request keeps its tokens, and the attention calls below give its
  * new rows no meaning; the caller repeats them in a later step. */
 int kda_pages_plan(const kda_pages* pg, int32_t n_slots, const int32_t* lens,
@@ -422,9 +425,9 @@ int kda_pages_plan(const kda_pages* pg, int32_t n_slots, const int32_t* lens,
                    int32_t* tables, int32_t* lens_out, int32_t* n_free_out, int32_t* cu,
                    int32_t* slots, int32_t* ok, void* stream);
 
-/* Write n rows (at most 2^24) of new keys and values into the pages of their
- * slots.  Slots are distinct; rows whose slot is negative or past the pool are skipped, and
- * everything else in the caches stays as it was.
+/* Write n rows (1 to 2^24) of new keys and values into the pages of their
+ * slots.  Slots are distinct; rows whose slot is negative or past the pool are
+ * skipped, and everything else in the caches stays as it was.
  * In:  k, v: n rows of [H_kv][d] with the given row strides; slots [n];
  *      k_scale, v_scale [H_kv] f32 (NULL = 1; NULL it must be unless the cache
  *      is KDA_E4M3): the cache holds
@@ -451,7 +454,8 @@ int kda_attn_step(const kda_attn_config* cfg, const void* q, int64_t q_stride,
                   const int32_t* lens, const float* k_scale, const float* v_scale, void* o,
                   float* lse, void* ws, void* stream);
 
-/* Write n latent rows into the pages of their slots (as kda_attn_append).
+/* Write n latent rows (1 to 2^24) into the pages of their slots (as
+ * kda_attn_append).
  * In:  c: n rows of d_c, r: n rows of d_r, with row strides; slots [n].
  * In/out: cache [n_pages][page][d_c + d_r]. */
 int kda_latent_append(const kda_latent_config* cfg, int32_t n, const void* c, int64_t c_stride,
@@ -491,7 +495,7 @@ size_t kda_latent_prefill_workspace_bytes(const kda_latent_config* cfg, int32_t 
  * A token whose c is not finite makes the rows that see it NaN, a row of w_uv
  * that is not finite its channel of all rows that have tokens.
  * Rows from min(cu[B], n) on are left as they were.
- * n, max_kv: at most 2^22.  max_kv is an upper bound of the tokens (lens) of
+ * n, max_kv: 1 to 2^22.  max_kv is an upper bound of the tokens (lens) of
  *      the requests that have rows, summed; the rows of requests past it are
  *      filled with NaN.  A request
  *      with more rows than tokens has its first rows filled with zeros.

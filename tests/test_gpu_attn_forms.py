@@ -28,6 +28,17 @@ def test_plan_of_many_pages(B, page, max_pages, most, spare, n_slots):
         assert got == want, [k for k in want if want[k] != got[k]]
 
 
+def test_plan_waiting_requests_behind_rows_past_the_slots():
+    # request 1's rows pass the slots: 2 and 4 wait behind them (0, nothing
+    # changes for them), 3 ends; before them request 0 waits (1)
+    page, lens, new = 16, [5, 3, 20, 17, 0], [0, 9, 0, -1, 0]
+    tables = [[0, -1], [1, -1], [2, 3], [4, 5], [-1, -1]]
+    free = [6, 7, -1, -1, -1, -1, -1, -1]
+    got = G._run_plan(K.Pages(5, page, 8, 2), lens, new, 2, free, tables, 4)
+    assert got["ok"] == [1, 0, 0, 1, 0] and got["lens"] == [5, 3, 20, 0, 0] and got["cu"] == [0, 0, 9, 9, 9, 9]
+    assert got["tables"] == tables and got["slots"] == [-1] * 4 and got["free"][:4] == [6, 7, 4, 5]
+
+
 @pytest.mark.parametrize("dtype,cache", [("bf16", "same"), ("f16", "e4m3")])
 @pytest.mark.parametrize("n,H,d,page", [(4099, 5, 128, 16), (2500, 7, 128, 256), (1100, 8, 256, 64)])
 def test_append_of_many_rows(dtype, cache, n, H, d, page):

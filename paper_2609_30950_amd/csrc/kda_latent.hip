@@ -159,6 +159,9 @@ __global__ void __launch_bounds__(256) k_latent_absorb(LatentArgs p) {
 // heads in eight waves read a row once less but load twice the queries before
 // they begin (whole steps, 64 heads, with 512 blocks either way: 8 requests up
 // to 8000 tokens 70 against 41 us, one of 4000 28 against 23).
+// The weights meet the values in 16 bits, their sum is float32: as pairs hi + lo
+// they would bring the error of 64 requests up to 8192 tokens in bf16 from
+// 1.78e-3 to 1.65e-3, the output's own rounding, and the step from 75.5 to 79 us.
 template <int F16, int DC, int DR, int NH>
 __global__ void __launch_bounds__(256, 2) k_latent_part(LatentArgs p) {
   constexpr int NW = 4;                           // waves

@@ -62,7 +62,6 @@ __device__ __forceinline__ uint4 keep_first(uint4 v, int n) {
 }
 
 constexpr float LN2 = 0.69314718055994530942f;
-constexpr float NEG_INF = -__builtin_huge_valf();
 
 }  // namespace
 

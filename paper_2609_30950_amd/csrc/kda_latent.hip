@@ -23,8 +23,6 @@ namespace kda {
 
 namespace {
 
-constexpr float NEG_INF = -__builtin_huge_valf();
-
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 

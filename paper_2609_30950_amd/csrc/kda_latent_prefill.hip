@@ -34,7 +34,6 @@ namespace kda {
 
 namespace {
 
-constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr int QT = PREFILL_ROWS;   // query rows of a block
 constexpr int KT = 64;    // tokens of a tile
 
@@ -73,35 +72,6 @@ __device__ __forceinline__ void row_range(const LatentPrefillArgs& p, int b, int
 }
 
 }  // namespace
-
-__device__ __forceinline__ int owner_of(const int32_t* off, int B, int i) {
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid] <= i) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
-// Exclusive prefix sums over the block's 256 threads, saturating at `most`.
-__device__ __forceinline__ int block_before(int v, int most, int* part) {
-  const int w = threadIdx.x / WAVE, lane = lane_id();
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x = min(x + y, most);
-  }
-  if (lane == WAVE - 1) part[w] = x;
-  const int left = __shfl_up(x, 1);
-  __syncthreads();
-  int before = lane ? left : 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < w) before = min(before + part[i], most);
-  return before;
-}
 
 // Bit i: row i of 32 rows of dc (256 or 512) elements holds one that is not
 // finite, the exponent's bits all set.  A load covers 512 elements.
@@ -151,18 +121,18 @@ __global__ void __launch_bounds__(256) k_latent_rows(LatentPrefillArgs p, int ro
     len[r] = cut_len(p.lens[b], cap);
     if (t * R + r >= B || first == last) len[r] = first = last = 0;
     tiles[r] = (last - first + QT - 1) / QT;
-    sum = min(sum + min(len[r], most), most);
+    sum = add_sat(sum, len[r]);
   }
   // the sum of the lengths decides who fits, the others count those who do
-  int at = block_before(sum, most, part[0]), pads = 0, qts = 0;
+  int all, at = block_before<256>(sum, part[0], all), pads = 0, qts = 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    at = min(at + min(len[r], most), most);
+    at = min(add_sat(at, len[r]), most);
     len[r] = at < most ? len[r] : -1;
     pads += len[r] > 0 ? (len[r] + 7) / 8 * 8 : 0;
     qts += tiles[r];
   }
-  int off = block_before(pads, 2147483647, part[1]), qoff = block_before(qts, 2147483647, part[2]);
+  int off = block_before<256>(pads, part[1], all), qoff = block_before<256>(qts, part[2], all);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int b = t * R + r;
@@ -190,7 +160,7 @@ __global__ void __launch_bounds__(256) k_latent_rows(LatentPrefillArgs p, int ro
   if (r >= (total + KT + 255) / 256 * 256) return;
   int src = 0;   // rows that hold no token: any row, masked where it is read
   if (r < total) {
-    const int b = owner_of(s_off, B, r), pos = r - s_off[b];
+    const int b = owner(s_off, B, r), pos = r - s_off[b];
     if (pos < s_kvn[b]) {
       const int pid = p.tables[(size_t)b * p.pg.max_pages + (pos >> p.sh)];
       src = (unsigned)pid < (unsigned)p.pg.n_pages ? (pid << p.sh) + (pos & (p.pg.page - 1)) : -1;
@@ -371,7 +341,7 @@ __global__ void __launch_bounds__(256 * TS, F16 || TS == 2 ? 1 : 2) k_latent_att
   const int32_t *off = p.lay, *kvn = p.lay + B + 1, *qoff = p.lay + 2 * B + 1;
   const int tiles = qoff[B], qt = tiles - 1 - (int)blockIdx.y;   // late tiles, the long ones, first
   if (qt < 0) return;
-  const int b = __builtin_amdgcn_readfirstlane(owner_of(qoff, B, qt));
+  const int b = __builtin_amdgcn_readfirstlane(owner(qoff, B, qt));
   int first, last;
   row_range(p, b, first, last);
   const int q0 = first + (qt - qoff[b]) * QT;                 // first row of the block

@@ -14,61 +14,6 @@ namespace {
 constexpr int PLAN_MAX_B = 4096;
 constexpr int PLAN_SLOTS = 4096;   // slots the planning block writes itself
 
-// Sums of counts saturate at 2^31 - 1: every count that matters is compared
-// with less.
-__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
-
-__device__ __forceinline__ int wave_incl_scan_sat(int v) {
-  v = add_sat(v, dpp_add_src<0x111, 0xF>(v));
-  v = add_sat(v, dpp_add_src<0x112, 0xF>(v));
-  v = add_sat(v, dpp_add_src<0x114, 0xF>(v));
-  v = add_sat(v, dpp_add_src<0x118, 0xF>(v));
-  v = add_sat(v, dpp_add_src<0x142, 0xA>(v));
-  v = add_sat(v, dpp_add_src<0x143, 0xC>(v));
-  return v;
-}
-
-// Sum of the other threads' values before this one's, and the total; `part`
-// has one slot per wave, used once.
-template <int NT>
-__device__ __forceinline__ int block_before(int v, int* part, int& total) {
-  constexpr int NW = NT / WAVE;
-  const int w = threadIdx.x / WAVE, lane = lane_id();
-  const int upto = wave_incl_scan_sat(v);
-  if (lane == WAVE - 1) part[w] = upto;
-  const int left = __shfl_up(upto, 1);
-  __syncthreads();
-  int before = lane ? left : 0;
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    if (i < w) before = add_sat(before, part[i]);
-    total = add_sat(total, part[i]);
-  }
-  return before;
-}
-
-// Last index whose (not decreasing) offset is at most i[k]: the request that
-// holds item i[k] of a packed list, whatever empty requests stand beside it.
-// N bisections side by side, in ceil(log2 B) steps.
-template <int N>
-__device__ __forceinline__ void owners(const int* off, int B, const int (&i)[N], int (&at)[N]) {
-#pragma unroll
-  for (int k = 0; k < N; ++k) at[k] = 0;
-  for (int step = B > 1 ? 1 << (31 - __builtin_clz(B - 1)) : 0; step > 0; step >>= 1)
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int to = min(at[k] + step, B - 1);
-      at[k] = off[to] <= i[k] ? max(at[k], to) : at[k];
-    }
-}
-__device__ __forceinline__ int owner(const int* off, int B, int i) {
-  const int x[1] = {i};
-  int at[1];
-  owners<1>(off, B, x, at);
-  return at[0];
-}
-
 __device__ __forceinline__ int place(const PlanArgs& p, int pid, int pos) {
   return (unsigned)pid < (unsigned)p.pg.n_pages ? (pid << p.sh) + (pos & (p.pg.page - 1)) : -1;
 }

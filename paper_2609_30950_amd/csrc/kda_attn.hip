@@ -14,9 +14,9 @@
 // operand of O^T.  With V stored eight tokens of a channel together, keys,
 // probabilities and values all go from memory to the matrix cores in
 // registers, without LDS.  The probabilities are pairs hi + lo in the second
-// product (a memory-bound kernel has the room: 143.8 us of a batch of 64 and 142.0
-// without; error against 64 bits 1.66e-3, the output's own rounding, and 1.77e-3
-// without).  The softmax is the running one (maximum and sum in
+// product (a memory-bound kernel has the room: 141.6 us of a batch of 64 with and
+// without, error against 64 bits 1.77e-3 without and 1.66e-3, the output's own
+// rounding, with).  The softmax is the running one (maximum and sum in
 // float32, one pass); waves and parts are joined by their maxima and sums,
 // which carry the factor of STEP_SHIFT with f16 elements.
 
@@ -157,21 +157,13 @@ __global__ void __launch_bounds__(256) k_attn_part(AttnArgs p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) split2<F16>(pr[2 * e], pr[2 * e + 1], hi[e], lo[e]);
     const uint4 pb = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    uint4 a[NT];
-    bool inf = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      a[i] = widen<F16>(vf[i]);
-      if (!full) a[i] = keep_first(a[i], nv);   // a zero weight does not hide Inf or NaN behind the end
-      if constexpr (!E8) inf = inf || not_finite<F16>(a[i]);   // the 8-bit type has no Inf
+      uint4 a = widen<F16>(vf[i]);
+      if (!full) a = keep_first(a, nv);   // a zero weight does not hide Inf or NaN behind the end
+      acc[i] = mma16<F16>(a, pl, acc[i]);
+      acc[i] = mma16<F16>(a, pb, acc[i]);
     }
-    // what the rounding left has either sign and may be zero: it must not meet an infinity
-    if (!__any(inf)) {
-#pragma unroll
-      for (int i = 0; i < NT; ++i) acc[i] = mma16<F16>(a[i], pl, acc[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i) acc[i] = mma16<F16>(a[i], pb, acc[i]);
   }
   ls = sum_groups(ls);
 

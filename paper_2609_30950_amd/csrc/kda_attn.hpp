@@ -143,15 +143,6 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
   lo = pack2<F16>(a - lo_f32<F16>(hi), b - hi_f32<F16>(hi));
 }
 
-// Of eight 16-bit elements: one is NaN or infinite (its exponent's bits are all
-// set, which the sum carries into the sign's place).
-template <int F16>
-__device__ __forceinline__ bool not_finite(const uint4& v) {
-  constexpr uint32_t EXP = F16 ? 0x7C007C00u : 0x7F807F80u, ONE = F16 ? 0x04000400u : 0x00800080u;
-  const uint32_t all = ((v.x & EXP) + ONE) | ((v.y & EXP) + ONE) | ((v.z & EXP) + ONE) | ((v.w & EXP) + ONE);
-  return (all & 0x80008000u) != 0u;
-}
-
 // D += A B for 16x16 tiles, K = 32: lane l supplies row l % 16 of A and
 // column l % 16 of B, each at k = 8 (l / 16) .. + 7; it receives rows
 // 4 (l / 16) + r of column l % 16.

@@ -74,9 +74,10 @@ __device__ __forceinline__ void row_range(const LatentPrefillArgs& p, int b, int
 }  // namespace
 
 // Bit i: row i of 32 rows of dc (256 or 512) elements holds one that is not
-// finite.  A load covers 512 elements.
+// finite, the exponent's bits all set.  A load covers 512 elements.
 template <int F16>
 __device__ __forceinline__ uint32_t not_finite_rows(const uint16_t* from, int dc) {
+  constexpr uint32_t EXP = F16 ? 0x7C007C00u : 0x7F807F80u, ONE = F16 ? 0x04000400u : 0x00800080u;
   const uint4* at = (const uint4*)from + lane_id();
   uint32_t bits = 0u;
   for (int i0 = 0; i0 < dc / 16; i0 += 16) {   // of the loads that the rows take, 16 or 32
@@ -85,7 +86,8 @@ __device__ __forceinline__ uint32_t not_finite_rows(const uint16_t* from, int dc
     for (int i = 0; i < 16; ++i) v[i] = at[WAVE * (i0 + i)];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const unsigned long long who = __ballot(not_finite<F16>(v[i]));
+      const uint32_t all = ((v[i].x & EXP) + ONE) | ((v[i].y & EXP) + ONE) | ((v[i].z & EXP) + ONE) | ((v[i].w & EXP) + ONE);
+      const unsigned long long who = __ballot((all & 0x80008000u) != 0u);
       if (dc == 512) bits |= (uint32_t)(who != 0) << (i0 + i);
       else bits |= (uint32_t)((uint32_t)who != 0u) << (2 * i) | (uint32_t)((who >> 32) != 0) << (2 * i + 1);
     }

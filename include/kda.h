@@ -346,10 +346,9 @@ int kda_prefill_aux(const kda_config* cfg, int32_t T, int32_t C, void* records,
  *   16-byte aligned, int32 and float32 arrays 4-byte aligned (KDA_ERR_ARG
  *   otherwise).
  * - Scores, softmax sums and accumulators are float32.  The probabilities meet
- *   the values in a 16-bit type; the sums they are divided by are not rounded.
- *   Their relative rounding is 2^-8 in bf16 and 2^-11 in f16, or 2^-16 and
- *   2^-22 where they are pairs hi + lo (kda_attn_step), and in f16 no less than
- *   2^-40 of the largest one (prompts: see there).
+ *   the values in a 16-bit type: relative rounding 2^-8 in bf16, and in f16
+ *   2^-11 down to 2^-29 of the largest one, below that 2^-40 of the largest
+ *   (prompts: see there); the sums they are divided by are not rounded.
  * - Counts are at least 1: a step without rows makes no call (KDA_ERR_ARG).
  * - Outputs and workspaces overlap no input but where it is said.  A call reads nothing that an
  *   earlier call left in a workspace.

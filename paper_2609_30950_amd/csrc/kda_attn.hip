@@ -13,10 +13,7 @@
 // eight consecutive tokens: exactly what it has to supply as the second
 // operand of O^T.  With V stored eight tokens of a channel together, keys,
 // probabilities and values all go from memory to the matrix cores in
-// registers, without LDS.  The probabilities are pairs hi + lo in the second
-// product (a memory-bound kernel has the room: 141.6 us of a batch of 64 with and
-// without, error against 64 bits 1.77e-3 without and 1.66e-3, the output's own
-// rounding, with).  The softmax is the running one (maximum and sum in
+// registers, without LDS.  The softmax is the running one (maximum and sum in
 // float32, one pass); waves and parts are joined by their maxima and sums,
 // which carry the factor of STEP_SHIFT with f16 elements.
 
@@ -153,15 +150,12 @@ __global__ void __launch_bounds__(256) k_attn_part(AttnArgs p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) pr[e] = step_weight<F16>(x[e] - ref);
     ls += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) split2<F16>(pr[2 * e], pr[2 * e + 1], hi[e], lo[e]);
-    const uint4 pb = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    const uint4 pb = make_uint4(pack2<F16>(pr[0], pr[1]), pack2<F16>(pr[2], pr[3]),
+                                pack2<F16>(pr[4], pr[5]), pack2<F16>(pr[6], pr[7]));
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       uint4 a = widen<F16>(vf[i]);
       if (!full) a = keep_first(a, nv);   // a zero weight does not hide Inf or NaN behind the end
-      acc[i] = mma16<F16>(a, pl, acc[i]);
       acc[i] = mma16<F16>(a, pb, acc[i]);
     }
   }

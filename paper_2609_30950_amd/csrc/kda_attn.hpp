@@ -136,13 +136,6 @@ __device__ __forceinline__ float hi_f32(uint32_t w) {
   return __builtin_bit_cast(float, w & 0xFFFF0000u);
 }
 
-// Two floats as pairs hi + lo of packed 16-bit values.
-template <int F16>
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = pack2<F16>(a, b);
-  lo = pack2<F16>(a - lo_f32<F16>(hi), b - hi_f32<F16>(hi));
-}
-
 // D += A B for 16x16 tiles, K = 32: lane l supplies row l % 16 of A and
 // column l % 16 of B, each at k = 8 (l / 16) .. + 7; it receives rows
 // 4 (l / 16) + r of column l % 16.

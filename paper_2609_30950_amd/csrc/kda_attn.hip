@@ -15,7 +15,12 @@
 // probabilities and values all go from memory to the matrix cores in
 // registers, without LDS.  The softmax is the running one (maximum and sum in
 // float32, one pass); waves and parts are joined by their maxima and sums,
-// which carry the factor of STEP_SHIFT with f16 elements.
+// which carry the factor of STEP_SHIFT with f16 elements.  The weights meet the
+// values in 16 bits, their sum is float32.  As pairs hi + lo they would bring the
+// error of 64 requests up to 8192 tokens in bf16 from 1.77e-3 to 1.66e-3, the
+// output's own rounding; an infinite value, of which a lo part makes NaN, then
+// needs a second pass over the part, and one request of 130000 tokens and a head
+// takes 24 us for 20.3 (the batch 142.7 for 141.9).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

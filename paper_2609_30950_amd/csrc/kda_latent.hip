@@ -492,13 +492,13 @@ hipError_t launch_part(const LatentArgs& a, hipStream_t st) {
 template <int F16, int DC, int DV>
 hipError_t launch_join(const LatentArgs& a, hipStream_t st) {
   // few blocks would each draw a whole head's weights through one compute unit
-  // (one request of 32 heads: 8.0 us with a block a head, 5.4 with four)
+  // (whole steps of one request, 32 heads: 22.6 us with a block a head, 19.8 with four)
   const dim3 grid((unsigned)a.H, (unsigned)((a.pg.B + 7) / 8));
   if (grid.x * grid.y < 256)
     return launch("latent_join", k_latent_join<F16, DC, DV, 32>, dim3(grid.x, grid.y, DV / 32), 1024, 0, st, a, 8);
   // two blocks a compute unit and more: half as many, which read the weights
-  // half as often (whole steps, 64 requests up to 2000 tokens, 64 heads: 64.3
-  // against 60.3 us; 128 requests, 128 heads: 129 against 107)
+  // half as often (whole steps, 64 requests up to 2000 tokens, 64 heads: 58.9
+  // against 54.6 us; 128 requests up to 1000, 128 heads: 134 against 112)
   if (grid.x * grid.y >= 512)
     return launch("latent_join", k_latent_join<F16, DC, DV, DV>, dim3(grid.x, (unsigned)((a.pg.B + 15) / 16)), 1024, 0,
                   st, a, 16);

@@ -313,9 +313,10 @@ __device__ __forceinline__ int key_swizzle(int r) { return (r / (16 / NC)) & (NC
 // that eight results of a lane in a row are eight consecutive tokens, the
 // operand of the product with the values, which lie eight tokens of a channel
 // together.  The scores of the next tile are formed beside the softmax of this
-// one.  Bound by the chip's power: 36 M pairs of 32 heads take 765 us (0.95
-// PFLOP/s) at 1.7 GHz with the matrix cores 56 % busy, against 786 us at 1.9
-// GHz and 44 % before the two overlapped.
+// one.  Bound by the clock, as if the chip's power were the limit: 36 M pairs of
+// 32 heads take 1.36 to 1.39 M cycles with the matrix cores 52 % busy, which are
+// 774 us at 1.8 GHz and 882 at 1.54 (0.94 and 0.83 PFLOP/s) in one run; before
+// the two overlapped 44 % and 786 us at 1.9 GHz.
 // With TS = 2 a block has two teams of four waves, which take the tiles in turn
 // and join their sums through LDS at the end: while there are fewer blocks than
 // the chip holds of the one-team form (512), it is the chain of a block's

@@ -377,6 +377,7 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
   constexpr int OS = DC + 8, PER = DC / WAVE / 4, VT = NV / 16, KP = 16 / VT;   // parts of d_c in the product
   __shared__ __align__(16) uint16_t mid[2][16 * OS];   // hi and lo
   __shared__ __align__(16) float sums[16][DC + 4];
+  __shared__ float total[16];                          // a request's sum of weights
   const int t = threadIdx.x, lane = lane_id(), m = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t / WAVE);
   const int h = blockIdx.x, b0 = rq * blockIdx.y, v0 = NV * blockIdx.z;
@@ -424,6 +425,7 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
       }
     }
     l = wave_sum_uniform(l);
+    if (s0 == 0 && lane == 0) total[w >> wl] = l;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const auto weight = [&](int s) {
       if (sp.ns <= WAVE) return bcast_f(mine.y, s) * inv;
@@ -471,6 +473,7 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
   if (kp == 0 && m < nb) {
 #pragma unroll
     for (int k = 1; k < KP; ++k) acc += *(const f32x4*)&sums[w + VT * k][4 * lane];
+    if (total[m] == 0.f) acc = f32x4{0.f, 0.f, 0.f, 0.f};   // no tokens: zero whatever the weights are
     uint2 y;
     y.x = pack2<F16>(acc[0], acc[1]);
     y.y = pack2<F16>(acc[2], acc[3]);

@@ -46,6 +46,22 @@ def test_prompts_value_weights_of_many_heads(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("B", [3, 70])
+def test_step_value_weights(dtype, B):
+    """As in prompts: the channel is NaN, and zero where there are no tokens."""
+    lens = [(0, 1, 90, 700)[b % 4] for b in range(B)]
+    s = _world(48, lens, 20, 64, 32, 256, dtype=dtype)
+    clean = _step(s)
+    s["w_uv"][3, 17, 100] = s["w_uv"][19, 63, 255] = float("nan")
+    some = torch.tensor(lens, device="cuda") > 0
+    want = clean.clone()
+    want[some, 3, 17] = want[some, 19, 63] = float("nan")
+    o = _step(s)
+    assert torch.equal(o.isnan(), want.isnan()) and torch.equal(o.nan_to_num(3.0), want.nan_to_num(3.0))
+    assert not bool(o[~some].any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("value", [INF, -INF, float("nan")])
 @pytest.mark.parametrize("lens,rows,at", [([150], [150], 100), ([3000], [5], 2997)], ids=str)
 def test_latent_vectors(dtype, value, lens, rows, at):

@@ -441,7 +441,6 @@ __global__ void __launch_bounds__(1024) k_latent_join(LatentArgs p, int rq) {
         for (int u = 0; u < PER; ++u) o[u] += ahead[i][u] * f;
       }
     }
-#pragma unroll 2
     for (int s = s0 + 4 * ds; s < sp.ns; s += ds) {
       const float f = weight(s);
 #pragma unroll
